@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kThreads, H::kBf16 ? 2 : 1) void attention_forward_
     f32x16 o[H::kBlocks];
 #pragma unroll
     for (int b = 0; b < H::kBlocks; ++b) o[b] = f32x16{};
-    float m = -INFINITY, l = 0.f;
+    float m = kNoReference, l = 0.f;
     auto add_keys = [&](uint32_t rows, bool diagonal) __attribute__((always_inline)) {
         attend<H>(at, rows, kValues + rows, q, c, diagonal, m, l, o);
     };

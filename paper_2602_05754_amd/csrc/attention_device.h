@@ -311,7 +311,9 @@ __device__ __forceinline__ void mask_later(f32x16& s) {
     for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + 4 * (lane >> 5) + i % 4 <= (lane & 31) ? s[i] : -INFINITY;
 }
 
-// Keys -> queries, 32 of each: softmax with a running reference m (of the exponents of 2), sum l and result o.
+// Keys -> queries, 32 of each: softmax with a running reference m (of the exponents of 2), sum l and result o.  The reference begins finite, below
+// all scores: of a query that has seen nothing but scores of -infinity the weights are 0, exp2(-infinity - m), and what comes counts in full.
+constexpr float kNoReference = -3.402823466e+38f;
 template <class H>
 __device__ __forceinline__ void attend(const Lane<H>& at, uint32_t keys, uint32_t values, const U4 (&q)[H::kSteps], float c, bool diagonal,
                                        float& m, float& l, f32x16 (&o)[H::kBlocks]) {

@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kThreads, Narrow<H>::kPerUnit) void attention_forwa
     f32x16 o[H::kBlocks];
 #pragma unroll
     for (int b = 0; b < H::kBlocks; ++b) o[b] = f32x16{};
-    float m = -INFINITY, l = 0.f;
+    float m = kNoReference, l = 0.f;
     auto fill = [&](int t, int buffer) __attribute__((always_inline)) {
         fill_tile<H>(k, a.k_stride, t * 32, w.rows, own_stage + buffer * 2 * N::kTile);
         fill_tile<H>(v, a.v_stride, t * 32, w.rows, own_stage + buffer * 2 * N::kTile + N::kTile);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads, Narrow<H>::kPerUnit) void attention_forwa
     lds_write<float>(own_stage + N::kStats + lane * 4, m);
     lds_write<float>(own_stage + N::kStats + 256 + lane * 4, l);
     __syncthreads();
-    float of_wave[kWaves], factor[kWaves], top = -INFINITY, sum = 0.f;
+    float of_wave[kWaves], factor[kWaves], top = kNoReference, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
         of_wave[i] = lds_read<float>(stages + uint32_t(i * N::kWave + N::kStats + lane * 4));
