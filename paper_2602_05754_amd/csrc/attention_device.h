@@ -324,9 +324,10 @@ __device__ __forceinline__ void attend(const Lane<H>& at, uint32_t keys, uint32_
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = with_other_half(top, [](float x, float y) { return fmaxf(x, y); }) * c;
     // The reference of the exponentials follows the maximum only when it has grown by 2^8 or more: sums and
-    // products stay within 2^8 of those with the maximum itself, and their quotient is the same.
+    // products stay within 2^8 of those with the maximum itself, and their quotient is the same.  A query's follows by its own scores, those
+    // of other queries in the tile leave its bits as they are.
     if (__any(top > m + 8.f)) {
-        const float next = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - next);
+        const float next = top > m + 8.f ? top : m, shrink = __builtin_amdgcn_exp2f(m - next);
         m = next;
         l *= shrink;
 #pragma unroll
