@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillCall a) {
         if (threadIdx.x == 0) a.loss[t] = 0.f;
         if (!dz) return;
         const float zero[kPer<T>] = {};
-        for (int c = threadIdx.x * kPer<T>; c < V; c += kThreads * kPer<T>) store_piece(dz + c, V - c, zero);
+        for (int64_t c = threadIdx.x * kPer<T>; c < V; c += kThreads * kPer<T>) store_piece(dz + c, V - c, zero);
     };
     if (weight == 0.f) return clear();
     const T minus_infinity = from_f32<T>(-INFINITY);

@@ -266,6 +266,25 @@ def test_distill_rows_that_are_not_read_and_masked_words(ctx, V):
     assert np.isnan(loss[0]) and np.isnan(dz[0]).all() and np.isfinite(dz[1:]).all()
 
 
+def test_distill_of_the_widest_rows(ctx):
+    """V = 2^31 - 4096, where a row's last step of 8192 words ends behind 2^31: a row that is read, between one without weight and one
+    without a teacher's word.  All logits are 0, so q = 1 / V and the sum of V ones in 32 bits is exact."""
+    V, T, room = (1 << 31) - 4096, 3, 8192
+    z = torch.zeros((T, V), dtype=torch.bfloat16, device="cuda")
+    buf = torch.full((room + T * V + room,), 3.0, dtype=torch.bfloat16, device="cuda")
+    dz = buf[room:room + T * V].view(T, V)
+    ids = torch.tensor([[V - 1], [V - 1], [V]], dtype=torch.int32, device="cuda")
+    loss = canary((T,), torch.float32)
+    tf.tf_distill_loss(ctx, T, V, 1, tf.TF_BF16, z, ids, torch.zeros((T, 1), device="cuda"), f32([0, 1, 1]), 1.0, 1024.0, loss, dz)
+    loss = host64(loss)
+    assert loss[0] == loss[2] == 0 and abs(loss[1] - np.log(V)) < 1e-5
+    every = lambda x, value: all(bool((part == value).all()) for part in x.split(1 << 28))
+    assert every(buf[:room], 3.0) and every(buf[room + T * V:], 3.0)
+    assert every(dz[0], 0.0) and every(dz[2], 0.0)
+    # (2^10 / V is 2^-21 within 2^-19 of it)
+    assert every(dz[1, :V - 1], 2.0 ** -21) and float(dz[1, V - 1]) == -1024.0
+
+
 # ---------------------------------------------------------------------------------------------
 # streams, graphs
 # ---------------------------------------------------------------------------------------------
