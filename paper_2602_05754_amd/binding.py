@@ -816,14 +816,15 @@ def _check_tensors(ctx, *wanted):
 
 def _workspace(ctx, workspace, n_bytes, stream):
     """(tensor to keep, address, bytes): the caller's workspace, or one made for this call by torch, in its
-    allocator's order for the call's stream."""
+    allocator's order for the call's stream, whichever is current."""
     if workspace is None:
         if ctx is None or n_bytes <= 0:
             return None, None, 0
         import torch
-        handle = _stream_handle(stream) or 0
-        with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=ctx.device_id)) if handle else contextlib.nullcontext():
-            workspace = torch.empty(n_bytes, dtype=torch.uint8, device=f"cuda:{ctx.device_id}")
+        handle, device = _stream_handle(stream) or 0, ctx.device_id
+        with contextlib.nullcontext() if handle == torch._C._cuda_getCurrentRawStream(device) else torch.cuda.stream(
+                torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)):
+            workspace = torch.empty(n_bytes, dtype=torch.uint8, device=f"cuda:{device}")
     if type(workspace) is int:
         return None, workspace, n_bytes                # the caller vouches for its size
     if not workspace.is_contiguous():

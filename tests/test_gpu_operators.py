@@ -331,3 +331,38 @@ def test_calls_on_another_stream_and_in_a_graph(ctx):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("default", [0, "stream"])
+def test_a_call_on_the_default_stream_while_another_is_current(ctx, default):
+    """Its workspace is not the other stream's memory, which that stream's work would get next."""
+    from paper_2602_05754_amd import binding
+    stream = 0 if default == 0 else torch.cuda.default_stream()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.empty(5 << 20, dtype=torch.uint8, device="cuda")             # the side stream's pool has memory of that size
+        keep, address, n = binding._workspace(ctx, None, 5 << 20, stream)
+        del keep
+        again = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        assert all(t.data_ptr() != address for t in again)
+    keep, address, n = binding._workspace(ctx, None, 5 << 20, side)
+    del keep
+    with torch.cuda.stream(side):
+        assert torch.empty(n, dtype=torch.uint8, device="cuda").data_ptr() == address
+
+
+def test_the_default_stream_gives_the_same_gradients_while_another_is_current(ctx):
+    rs = np.random.default_rng(4)
+    T, V, d = 900, 60, 264
+    _, dout = stored(rs.standard_normal((T, d)), "bf16")
+    ids = torch.from_numpy(ids_of("text", T, V, rs).astype(np.int32)).cuda()
+    want, got = torch.empty((V, d), device="cuda"), torch.empty((V, d), device="cuda")
+    tf.tf_embedding_backward(ctx, T, V, d, tf.TF_BF16, ids, dout, 1.0, want, tf.TF_F32)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for _ in range(20):
+            tf.tf_embedding_backward(ctx, T, V, d, tf.TF_BF16, ids, dout, 1.0, got, tf.TF_F32, stream=0)
+            torch.empty(tf.tf_embedding_workspace(T, V, d), dtype=torch.uint8, device="cuda").fill_(255)       # the current stream's own work
+        torch.cuda.synchronize()
+    assert torch.equal(got, want)

@@ -193,3 +193,36 @@ def test_the_attention_wrappers_look_at_their_tensors():
                 dict(io=BF16), dict(v=new(10, 128)[:, ::2]), dict(q=new(10, 4, 32).double())):
         with pytest.raises(ValueError):
             call(**bad)
+
+
+@pytest.mark.parametrize("asked,current,want", [(None, 0, 0), (None, 7, 7), (0, 0, 0), (0, 7, 0), (7, 0, 7), (9, 7, 9), ("default", 7, 0), ("side", 0, 5), ("side", 5, 5)])
+def test_a_workspace_comes_from_the_pool_of_the_calls_stream(monkeypatch, asked, current, want):
+    """Whichever stream is current: torch hands its memory out again in that stream's order."""
+    import contextlib
+    import types
+    import torch
+    from paper_2602_05754_amd import binding
+    stream = lambda handle: types.SimpleNamespace(cuda_stream=handle)
+    now, made, empty = [current], [], torch.empty
+
+    @contextlib.contextmanager
+    def inside(s):
+        now.append(s.cuda_stream)
+        yield
+        now.pop()
+
+    def new(*a, device, **k):
+        assert device == "cuda:3"
+        made.append(now[-1])
+        return empty(*a, **k)
+    monkeypatch.setattr(torch, "empty", new)
+    for name, value in (("current_stream", lambda device=None: stream(now[-1])), ("default_stream", lambda device=None: stream(0)), ("stream", inside),
+                        ("ExternalStream", lambda handle, device=None: stream(handle)), ("current_device", lambda: 3)):
+        monkeypatch.setattr(torch.cuda, name, value)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: now[-1], raising=False)
+    asked = {"default": stream(0), "side": stream(5)}.get(asked, asked) if isinstance(asked, str) else asked
+    ctx = types.SimpleNamespace(device_id=3)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 3)
+    keep, address, n = binding._workspace(ctx, None, 64, asked)
+    assert made == [want] and now == [current] and n == 64 and address == keep.data_ptr()
+    assert binding._stream_handle(asked) == (want or None)             # where the kernels go
