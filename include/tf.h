@@ -543,7 +543,8 @@ double tf_actual_freeze_ratio(double r, int64_t t, int64_t T_m, int64_t T_f);
  *
  * Workspaces: some calls need device memory for the call's duration.  The caller
  * gives it, 16-byte aligned, and its size; the tf_*_workspace functions (host only)
- * return the bytes that a call of these sizes needs, or a negative tf_status.  Its
+ * return the bytes that a call of these sizes needs, or a negative tf_status; calls with
+ * fewer tokens need no more, so the largest call's workspace does for them all.  Its
  * contents mean nothing before and after a call; calls on one stream may share it.
  * Too small a workspace is TF_ERR_WORKSPACE.
  */

@@ -259,13 +259,21 @@ void backward(hipStream_t stream, const NormRows& r, int blocks) {
 
 }  // namespace
 
-int norm_backward_blocks(int64_t T, int d) {
+// Groups of rows that the blocks of a backward take one after the other.
+static int64_t backward_groups(int64_t T, int d) {
     int rows = 1;
     with_shape<float, kBackwardThreads>(d, [&](auto shape) { rows = decltype(shape)::kRows; });
-    // as few blocks as take the same number of rounds: each leaves two rows of sums
-    const int64_t groups = (T + rows - 1) / rows, rounds = (groups + kNormBlocks - 1) / kNormBlocks;
+    return (T + rows - 1) / rows;
+}
+
+// As few blocks as take the same number of rounds: each leaves two rows of sums.
+static int backward_blocks(int64_t T, int d) {
+    const int64_t groups = backward_groups(T, d), rounds = (groups + kNormBlocks - 1) / kNormBlocks;
     return int((groups + rounds - 1) / rounds);
 }
+
+// The most blocks of any call with up to T rows: 300 rows take fewer than 256 do, and a workspace for the one has to do for the other.
+int norm_backward_most_blocks(int64_t T, int d) { return int(std::min<int64_t>(backward_groups(T, d), kNormBlocks)); }
 
 hipError_t launch_norm_forward(hipStream_t stream, const NormRows& r, Dtype dtype) {
     dtype == Dtype::BF16 ? forward<uint16_t>(stream, r) : forward<float>(stream, r);
@@ -273,7 +281,7 @@ hipError_t launch_norm_forward(hipStream_t stream, const NormRows& r, Dtype dtyp
 }
 
 hipError_t launch_norm_backward(hipStream_t stream, const NormRows& r, Dtype dtype, Dtype dw_dtype, bool accumulate) {
-    const int blocks = norm_backward_blocks(r.T, r.d);
+    const int blocks = backward_blocks(r.T, r.d);
     dtype == Dtype::BF16 ? backward<uint16_t>(stream, r, blocks) : backward<float>(stream, r, blocks);
     if (r.dw || r.db)
         hipLaunchKernelGGL(norm_sum_kernel, dim3((r.d + 63) / 64, 2), dim3(64 * kSumWaves), 0, stream, r, blocks, dw_dtype == Dtype::BF16, accumulate);

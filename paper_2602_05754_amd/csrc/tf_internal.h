@@ -298,7 +298,7 @@ struct NormRows {
 };
 constexpr int kNormMaxWidth = 16384;
 constexpr int kNormBlocks = 256;        // of a backward, at most: each leaves a row of partial sums
-int norm_backward_blocks(int64_t T, int d);
+int norm_backward_most_blocks(int64_t T, int d);
 hipError_t launch_norm_forward(hipStream_t stream, const NormRows& r, Dtype dtype);
 hipError_t launch_norm_backward(hipStream_t stream, const NormRows& r, Dtype dtype, Dtype dw_dtype, bool accumulate);
 

@@ -272,7 +272,7 @@ int tf_attention_backward(tf_ctx* ctx, void* hip_stream, int32_t n_seqs, const i
 
 int64_t tf_norm_workspace(int64_t T, int64_t d) {
     if (check_norm(T, d, 0) != TF_OK) return check_norm(T, d, 0);
-    return 2 * int64_t(norm_backward_blocks(T, int(d))) * d * 4;
+    return 2 * int64_t(norm_backward_most_blocks(T, int(d))) * d * 4;
 }
 
 int tf_norm_forward(tf_ctx* ctx, void* hip_stream, int64_t T, int64_t d, tf_dtype io_dtype,

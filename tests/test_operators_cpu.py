@@ -226,3 +226,20 @@ def test_a_workspace_comes_from_the_pool_of_the_calls_stream(monkeypatch, asked,
     keep, address, n = binding._workspace(ctx, None, 64, asked)
     assert made == [want] and now == [current] and n == 64 and address == keep.data_ptr()
     assert binding._stream_handle(asked) == (want or None)             # where the kernels go
+
+
+def test_a_workspace_does_for_all_smaller_calls():
+    for d in (1, 64, 1000, 1024, 1500, 2731, 4096, 8192, 16384):
+        sizes = [tf.tf_norm_workspace(T, d) for T in list(range(1, 1100)) + [2047, 2048, 2049, 4097, 5000, 1 << 20, (1 << 31) - 4096]]
+        assert sizes == sorted(sizes), d
+        # what a call is given is what it asks for
+        lib = tf.load_library()
+        raw = lambda T, n: lib.tf_norm_backward(None, None, T, d, BF16, A, A << 20, A << 21, A << 22, A << 23, 1, A << 24, A << 25, A << 26, BF16, 0, A << 27, n)
+        assert raw(300, tf.tf_norm_workspace(300, d)) == INVALID and raw(300, sizes[-1]) == INVALID and raw(300, 4 * d) == WORKSPACE
+    lengths = list(range(1, 600)) + [8191, 8192, 8193, 16384, 16385, 30000, 1 << 20, (1 << 31) - 4096]
+    for d in (1, 7, 8, 4096):
+        sizes = [tf.tf_embedding_workspace(T, 1000, d) for T in lengths]
+        assert sizes == sorted(sizes), d
+    for hq, hkv, d in ((1, 1, 16), (32, 8, 128), (3, 1, 48)):
+        sizes = [tf.tf_attention_workspace(T, hq, hkv, d, BF16) for T in lengths]
+        assert sizes == sorted(sizes)
