@@ -192,7 +192,9 @@ __global__ __launch_bounds__(kThreads, H::kBf16 ? 2 : 1) void attention_dq_kerne
         fill_stage<H>(k, a.k_stride, t * kStageRows, w.rows, stages + stage);
         fill_stage<H>(v, a.v_stride, t * kStageRows, w.rows, stages + kValues + stage);
     }, [&](uint32_t rows, bool diagonal) __attribute__((always_inline)) {
-        add_product<H>(at, rows, gradient(rows, diagonal), dq);
+        const f32x16 ds = gradient(rows, diagonal);
+        add_product<H>(at, rows, ds, dq);
+        if (diagonal && w.rows <= kShort) add_rest<H>(at, rows, ds, dq);
     });
     settle<H>(dq);
     T* out = static_cast<T*>(a.dq) + token * a.q_stride + w.head * H::kD;
@@ -292,7 +294,9 @@ __global__ __launch_bounds__(KeyBlock<H>::kThreads, KeyBlock<H>::kPairs ? 2 : Ke
         weights(stage, part, query0, masked, p, ds);
         const uint32_t rows = stage * H::kStage + part * H::kPitch;
         add_product<H>(at, kGrads + rows, p, dv);
+        if (masked && w.rows <= kShort) add_rest<H>(at, kGrads + rows, p, dv);
         add_product<H>(at, rows, ds, dk);
+        if (masked && w.rows <= kShort) add_rest<H>(at, rows, ds, dk);
     };
     // Stages of queries: of all heads the masked ones (the two of the block's own rows and the last one, if it is not whole), then
     // of all heads the others, of which every wave takes all.  (Both kinds in one loop cost the compiler copies of the sums.)

@@ -185,8 +185,10 @@ __device__ __forceinline__ void add_product(const Lane<H>& lane, uint32_t at, co
     }
 }
 
-// acc^T += X^T (what rounding to bf16 has taken from w).  For the gradients of sequences of one tile, where few terms leave a rounding as it is
-// (the largest error of dq and dk in 144 small calls, against that of 32-bit products: 1.7 times, so 1.3), and which take no longer for it.
+// acc^T += X^T (what rounding to bf16 has taken from w).  For the gradients of sequences of one tile, on all kernels: what a sequence gets does not
+// depend on those that it is packed with.  Root mean square error, heads of 64 and 128, over that of 32-bit products rounded once: dq and dk 1.42,
+// dv 1.25 to 1.39 at any length from 4 to 256; with this 1.00.  us, backward, 100 sequences of 20 tokens, 32 / 8 heads of 64 and 128:
+// 53 92, with this 56 101; calls without such sequences take no longer.  In sequences of more tiles it would be four more products to the seven.
 template <class H>
 __device__ __forceinline__ void add_rest(const Lane<H>& lane, uint32_t at, const f32x16& w, f32x16 (&acc)[H::kBlocks]) {
     if constexpr (H::kBf16) {
@@ -200,7 +202,7 @@ __device__ __forceinline__ void add_rest(const Lane<H>& lane, uint32_t at, const
         add_product<H>(lane, at, rest, acc);
     }
 }
-constexpr int kShort = 32;                 // rows of such a sequence
+constexpr int kShort = 32;                 // rows of such a sequence, at most
 
 // One block of 32 columns of such a product, each element of X multiplied only where keep(row of the tile, column of w) holds.
 template <class H, class F>
