@@ -188,7 +188,7 @@ __device__ __forceinline__ void add_product(const Lane<H>& lane, uint32_t at, co
 // acc^T += X^T (what rounding to bf16 has taken from w).  For the gradients of sequences of one tile, on all kernels: what a sequence gets does not
 // depend on those that it is packed with.  Root mean square error, heads of 64 and 128, over that of 32-bit products rounded once: dq and dk 1.42,
 // dv 1.25 to 1.39 at any length from 4 to 256; with this 1.00.  us, backward, 100 sequences of 20 tokens, 32 / 8 heads of 64 and 128:
-// 53 92, with this 56 101; calls without such sequences take no longer.  In sequences of more tiles it would be four more products to the seven.
+// 53 92, with this 56 101; calls without such sequences take no longer.  In sequences of more tiles it would be three more products to the seven.
 template <class H>
 __device__ __forceinline__ void add_rest(const Lane<H>& lane, uint32_t at, const f32x16& w, f32x16 (&acc)[H::kBlocks]) {
     if constexpr (H::kBf16) {
