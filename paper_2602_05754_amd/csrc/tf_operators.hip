@@ -12,20 +12,23 @@ using namespace tf;
 inline uintptr_t address(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 4096;
 
-// The tensors of a call: each required or not, its bytes, read or written.
+// The tensors of a call: each required or not, its bytes, read or written.  Takes no memory: nothing here can throw.
 struct Tensors {
-    std::vector<ByteRange> ranges;
-    int status = TF_OK;
+    ByteRange ranges[10];
+    int n = 0, status = TF_OK;
     void add(const void* p, int64_t bytes, bool output, bool required = true) {
         if (status != TF_OK) return;
         if (!p) { if (required) status = TF_ERR_INVALID_ARG; return; }
         if (!aligned16(p)) { status = TF_ERR_ALIGN; return; }
-        ranges.push_back({address(p), address(p) + uintptr_t(bytes), output});
+        ranges[n++] = {address(p), address(p) + uintptr_t(bytes), output};
     }
     void in(const void* p, int64_t bytes, bool required = true) { add(p, bytes, false, required); }
     void out(const void* p, int64_t bytes, bool required = true) { add(p, bytes, true, required); }
     int check() {
-        if (status == TF_OK && outputs_overlap_something(ranges)) status = TF_ERR_ALIAS;
+        for (int i = 0; i < n; ++i)
+            for (int j = 0; j < i; ++j)
+                if (status == TF_OK && (ranges[i].output || ranges[j].output) && ranges[i].lo < ranges[j].hi && ranges[j].lo < ranges[i].hi)
+                    status = TF_ERR_ALIAS;
         return status;
     }
 };

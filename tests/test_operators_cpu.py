@@ -243,3 +243,57 @@ def test_a_workspace_does_for_all_smaller_calls():
     for hq, hkv, d in ((1, 1, 16), (32, 8, 128), (3, 1, 48)):
         sizes = [tf.tf_attention_workspace(T, hq, hkv, d, BF16) for T in lengths]
         assert sizes == sorted(sizes)
+
+
+REFUSING = """
+#include <cstdlib>
+#include <new>
+static bool refuse = false;
+extern "C" void refuse_memory(int on) { refuse = on; }
+void* operator new(std::size_t n) { if (!refuse) if (void* p = std::malloc(n ? n : 1)) return p; throw std::bad_alloc(); }
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, std::size_t) noexcept { std::free(p); }
+"""
+CALLS = """
+import ctypes, sys
+from ctypes import c_float as f, c_int64 as i, c_void_p
+memory, lib = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL), ctypes.CDLL(sys.argv[2])
+p = lambda n: c_void_p(n << 20)
+starts = (i * 3)(0, 4, 10)
+rows = [p(1), i(128), p(2), i(64), p(3), i(64)]
+calls = {
+    "norm_forward": (i(8), i(16), 0, p(1), p(2), p(3), f(1e-5), 1, p(4), p(5), p(6)),
+    "norm_backward": (i(8), i(16), 0, p(1), p(2), p(3), p(4), p(5), 1, p(6), p(7), p(8), 0, 0, p(9), i(1 << 20)),
+    "embedding_forward": (i(8), i(32), i(16), 0, p(1), p(2), f(1), p(3)),
+    "embedding_backward": (i(8), i(32), i(16), 0, p(1), p(2), f(1), p(3), 0, 0, p(4), i(1 << 20)),
+    "distill_loss": (i(4), i(50), i(3), 0, p(1), p(2), p(3), p(4), f(1), f(1), p(5), p(6)),
+    "attention_forward": (2, starts, i(10), 4, 2, 32, 0, *rows, f(0.2), p(4), i(128), p(5)),
+    "attention_backward": (2, starts, i(10), 4, 2, 32, 0, *rows, p(4), i(128), p(5), p(6), f(0.2), p(7), p(8), p(9), p(10), i(1 << 20)),
+}
+for name, args in calls.items():
+    call = lambda: getattr(lib, "tf_" + name)(None, None, *args)
+    before = call()
+    memory.refuse_memory(1)
+    code = call()
+    memory.refuse_memory(0)
+    print(name, before, code, call(), flush=True)
+"""
+
+
+def test_no_exception_leaves_a_call_without_memory(tmp_path):
+    """Host memory that cannot be had is an error code, or none where the call needs none; in a process of its own."""
+    import subprocess
+    import sys
+    from paper_2602_05754_amd import binding
+    tf.load_library()
+    source, shim = tmp_path / "refusing.cpp", tmp_path / "refusing.so"
+    source.write_text(REFUSING)
+    subprocess.run(["g++", "-shared", "-fPIC", str(source), "-o", str(shim)], check=True)
+    res = subprocess.run([sys.executable, "-c", CALLS, str(shim), binding._LIB_PATH], capture_output=True, text=True, timeout=100)
+    assert res.returncode == 0, res.stdout + res.stderr
+    lines = [line.split() for line in res.stdout.splitlines()]
+    assert len(lines) == 7
+    for name, before, refused, after in lines:
+        assert int(before) == int(after) == INVALID, name                  # only the missing context
+        assert int(refused) in (INVALID, WORKSPACE), name
+    assert any(int(refused) == WORKSPACE for _, _, refused, _ in lines)    # the memory was refused
