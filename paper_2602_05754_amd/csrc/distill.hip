@@ -12,7 +12,8 @@
 // us and logical GB/s (copies run at 5000), bf16, K = 32: 4096 rows of 65536 205, 5230 (two blocks to a compute unit); 2048 of 131072 239,
 // 4490 (one: a row fills the registers, and nothing is read while it is written); 2048 of 160000 291, 4500.
 // Exponentials are of (z - maximum) / tau, the difference first: z / tau of a word masked with the type's lowest value
-// need not be finite, and where q is large the difference is exact.
+// need not be finite, and where q is large the difference is exact.  The loss adds up tau log p and tau log q for the same reason: log q of such
+// a word is not finite at a temperature below 1, tau^2 log q is.
 #include "row_device.h"
 
 #include <algorithm>
@@ -148,15 +149,16 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillCall a) {
     const float log_sum = logf(sum), inv_sum = 1.f / sum;
 
     if (threadIdx.x < 64) {
+        const float factor = weight * a.temperature;
         float l = 0.f;
         for (int k = threadIdx.x; k < K; k += 64) {
-            const float logp = (p[k] - tmax) * inv_tau - log_tsum, pk = expf(logp);
+            const float pk = expf((p[k] - tmax) * inv_tau - log_tsum);
             if (pk == 0.f) continue;                   // nothing of an absent or hopeless entry, whatever log q is
-            const float logq = (z_of[k] - top) * inv_tau - log_sum;
-            l += pk * (logp - logq);
+            const float tau_logp = (p[k] - tmax) - a.temperature * log_tsum, tau_logq = (z_of[k] - top) - a.temperature * log_sum;
+            l += pk * factor * (tau_logp - tau_logq);
         }
         l = wave_sum(l);
-        if (threadIdx.x == 0) a.loss[t] = weight * (a.temperature * a.temperature) * l;
+        if (threadIdx.x == 0) a.loss[t] = l;
     }
     if (!dz) return;
     const float scale = a.grad_scale * weight * a.temperature;

@@ -266,6 +266,28 @@ def test_distill_rows_that_are_not_read_and_masked_words(ctx, V):
     assert np.isnan(loss[0]) and np.isnan(dz[0]).all() and np.isfinite(dz[1:]).all()
 
 
+@pytest.mark.parametrize("tau", [0.01, 0.25, 0.5, 0.99, 1.0])
+@pytest.mark.parametrize("io", TYPES)
+def test_distill_of_a_word_with_the_lowest_value(ctx, io, tau):
+    """A word that the teacher names and the student's mask rules out: log q = z / tau is beyond 32 bits, the loss tau^2 p log q is not.
+    Of the sum only that word's term is left, its factors rounded a few times each; the gradient does not see how low the word is."""
+    rs = np.random.default_rng(5)
+    lowest = float(torch.finfo(TDT[io]).min)
+    z = rs.standard_normal((4, 60))
+    z[:, 7] = lowest
+    z[2] = lowest                                      # all but one
+    z[2, 30] = 1.0
+    z, gz = stored(z, io)
+    ids, teacher = np.tile([7, 9, 11], (4, 1)), rs.standard_normal((4, 3)).astype(np.float32)
+    teacher[3, 0] = -np.inf                            # there the teacher has ruled it out too
+    tau = float(np.float32(tau))
+    loss, dz = distill(ctx, gz, ids, teacher, None, tau, 1.0, io)
+    el, ez = op.distill_loss(z, ids, teacher, None, tau, 1.0)
+    assert np.isfinite(el).all() and np.all(np.abs(loss - el) <= 1e-4 * np.abs(el)), (loss, el)
+    # exp of up to 10 / tau, rounded to 24 bits as the arguments are; bf16: the result's rounding
+    assert np.all(np.abs(dz - ez) <= (2.0 ** -8 if io == "bf16" else 0) * np.abs(ez) + tau * (20 / tau) * 2.0 ** -22)
+
+
 def test_distill_of_the_widest_rows(ctx):
     """V = 2^31 - 4096, where a row's last step of 8192 words ends behind 2^31: a row that is read, between one without weight and one
     without a teacher's word.  All logits are 0, so q = 1 / V and the sum of V ones in 32 bits is exact."""
