@@ -639,7 +639,7 @@ int tf_embedding_backward(tf_ctx* ctx, void* hip_stream, int64_t T, int64_t n_ro
  *               outside [0, V) is absent; an id that is named twice counts with both.
  *   token_weight   device, T floats, or NULL (all 1).  Where it is 0, or no entry of a row has
  *               any probability, the loss is 0, the gradient is zeros and the logits are not read.
- *   temperature    finite, > 0.       grad_scale   finite.
+ *   temperature    finite, at least 2^-126 (below, 1 / temperature is beyond 32 bits).       grad_scale   finite.
  *   loss        T floats.     dlogits   io_dtype, NULL: the loss alone.
  */
 int tf_distill_loss(tf_ctx* ctx, void* hip_stream, int64_t T, int64_t V, int64_t K, tf_dtype io_dtype,

@@ -2,6 +2,7 @@
 // Declarations and contracts: include/tf.h.
 #include "tf_context.h"
 
+#include <cfloat>
 #include <cmath>
 #include <new>
 
@@ -398,7 +399,7 @@ int tf_distill_loss(tf_ctx* ctx, void* hip_stream, int64_t T, int64_t V, int64_t
                     float temperature, float grad_scale, float* loss, void* dlogits) {
     if (!valid_dtype(io_dtype)) return TF_ERR_DTYPE;
     if (T <= 0 || T > kMaxTokens || V <= 0 || V > kMaxTokens || K <= 0 || K > kDistillMaxK) return TF_ERR_SHAPE;
-    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(grad_scale)) return TF_ERR_INVALID_ARG;
+    if (!(temperature >= FLT_MIN) || !std::isfinite(temperature) || !std::isfinite(grad_scale)) return TF_ERR_INVALID_ARG;
     const int64_t e = size_of(io_dtype);
     Tensors t;
     t.in(logits, T * V * e);

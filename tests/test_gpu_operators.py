@@ -288,6 +288,17 @@ def test_distill_of_a_word_with_the_lowest_value(ctx, io, tau):
     assert np.all(np.abs(dz - ez) <= (2.0 ** -8 if io == "bf16" else 0) * np.abs(ez) + tau * (20 / tau) * 2.0 ** -22)
 
 
+@pytest.mark.parametrize("tau", [2.0 ** -126, 2.0 ** -100, 2.0 ** -40])
+def test_distill_at_the_smallest_temperatures(ctx, tau):
+    """p and q have one word each: the loss is tau times the difference of two logits, the gradient tau at the two words."""
+    rs = np.random.default_rng(6)
+    z, teacher = rs.standard_normal((5, 300)).astype(np.float32), rs.standard_normal((5, 4)).astype(np.float32)
+    ids = np.tile([7, 9, 11, 250], (5, 1))
+    loss, dz = distill(ctx, f32(z), ids, teacher, None, tau, 1.0, "f32")
+    el, ez = op.distill_loss(z, ids, teacher, None, tau, 1.0)
+    assert np.all(np.abs(loss - el) <= 1e-5 * el) and np.array_equal(dz, ez) and (ez != 0).any()
+
+
 def test_distill_of_the_widest_rows(ctx):
     """V = 2^31 - 4096, where a row's last step of 8192 words ends behind 2^31: a row that is read, between one without weight and one
     without a teacher's word.  All logits are 0, so q = 1 / V and the sum of V ones in 32 bits is exact."""

@@ -297,3 +297,12 @@ def test_no_exception_leaves_a_call_without_memory(tmp_path):
         assert int(before) == int(after) == INVALID, name                  # only the missing context
         assert int(refused) in (INVALID, WORKSPACE), name
     assert any(int(refused) == WORKSPACE for _, _, refused, _ in lines)    # the memory was refused
+
+
+def test_distill_refuses_a_temperature_whose_inverse_is_infinite():
+    call = lambda tau: code(tf.tf_distill_loss, None, 4, 50, 3, F32, A, 2 * A, 3 * A, None, tau, 1.0, 4 * A, None)
+    lib = tf.load_library()
+    assert call(1e-39) == call(1e-45) == INVALID
+    # (without a context those are -1 in any case: a misaligned tensor, which is looked at later, tells them apart)
+    raw = lambda tau, ids: lib.tf_distill_loss(None, None, 4, 50, 3, F32, A, ids, 3 * A, None, tau, 1.0, 4 * A, None)
+    assert raw(1e-39, A + 4) == INVALID and raw(2.0 ** -126, A + 4) == ALIGN and raw(1e-30, A + 4) == ALIGN
