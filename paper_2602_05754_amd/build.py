@@ -78,7 +78,7 @@ def scc_hazards(asm_text: str) -> list:
 
 # Wait states between a matrix instruction and the first other instruction that reads its result, by the
 # passes it takes (f64 16x16x4: 16, and LDS reads need 18; fp32 16x16x4: 8, 32x32x2: 16; bf16 16x16x32: 4, 32x32x16: 8).
-# The passes count too: a matrix instruction begins when the one before it has had the unit for them.
+# The passes count too: a matrix instruction begins when the one before it has had the unit for them, a state each.
 _MFMA_WAIT = (("f64", 18, 16), ("16x16x4_f32", 10, 8), ("32x32x2_f32", 18, 16), ("32x32x16_bf16", 12, 8), ("", 8, 4))
 _REGISTERS = re.compile(r"\b([va])(?:(\d+)|\[(\d+):(\d+)\])")
 _VECTOR_OPS = ("v_", "ds_", "global_", "buffer_", "flat_", "scratch_")
@@ -147,8 +147,8 @@ def mfma_hazards(asm_text: str) -> list:
                 elif op.startswith("v_mfma"):
                     need, passes = next((n, p) for key, n, p in _MFMA_WAIT if key in op)
                     last = state.pop(None, None)
-                    if last is not None and last[0] < last[1]:     # it waits for the unit
-                        states += last[1] - last[0]
+                    if last is not None and last[0] < last[1]:     # it waits for the unit: it is the passes' next state itself
+                        states += last[1] - last[0] - 1
                     written = {r: (0, need) for r in _registers(operands[:1])}
                     written[None] = (0, passes)
                 elif op.startswith(_VECTOR_OPS):

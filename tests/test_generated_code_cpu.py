@@ -41,3 +41,48 @@ def test_paths_through_branches_and_loops_are_followed():
     assert found(".LBB0_1:", READ, MFMA, WAIT, "s_cbranch_scc1 .LBB0_1") == []
     assert found(MFMA, "s_cbranch_scc1 .LBB0_3", WAIT, "s_branch .LBB0_4", ".LBB0_3:", "v_mov_b32_e32 v1, v2", ".LBB0_4:", READ) == [READ]
     assert found(MFMA, "s_branch .LBB0_4", ".LBB0_3:", READ, ".LBB0_4:", "v_mov_b32_e32 v1, v2") == []
+
+
+SHAPES = {"v_mfma_f32_32x32x16_bf16": (12, 8), "v_mfma_f32_32x32x2_f32": (18, 16), "v_mfma_f32_16x16x4_f32": (10, 8),
+          "v_mfma_f32_16x16x32_bf16": (8, 4), "v_mfma_f64_16x16x4_f64": (18, 16)}
+
+
+def matrix(op, first, last):
+    return f"{op} v[{first}:{last}], v[200:203], v[204:207], v[{first}:{last}]"
+
+
+@pytest.mark.parametrize("op", ["v_mfma_f32_32x32x16_bf16", "v_mfma_f32_32x32x2_f32"])
+def test_the_tiles_of_32_rows_have_their_number_of_states(op):
+    need, read = SHAPES[op][0], "v_mov_b32_e32 v120, v15"
+    assert found(matrix(op, 0, 15), *["s_nop 0"] * need, read) == []
+    assert found(matrix(op, 0, 15), *["s_nop 0"] * (need - 1), read) == [read]
+    assert found(matrix(op, 0, 15).replace("v[0:15]", "a[0:15]"), "v_accvgpr_read_b32 v9, a7") == ["v_accvgpr_read_b32 v9, a7"]
+
+
+@pytest.mark.parametrize("second", SHAPES)
+@pytest.mark.parametrize("first", SHAPES)
+def test_a_matrix_instruction_waits_for_the_one_before(first, second):
+    """Right behind another it begins when that one has had the unit for its passes: those states have gone by with it, and no more."""
+    need, passes = SHAPES[first]
+    read = "v_mov_b32_e32 v120, v15"
+    for between in (0, 1, passes // 2, passes - 1, passes, passes + 1):        # states between the two
+        gone = max(between + 1, passes)                                        # when the second has been issued
+        lines = [matrix(first, 0, 15)] + ["s_nop 0"] * between + [matrix(second, 32, 47)]
+        left = max(need - gone, 0)
+        assert found(*lines, *["s_nop 0"] * left, read) == []
+        if left:
+            assert found(*lines, *["s_nop 0"] * (left - 1), read) == [read]
+
+
+def test_waits_and_barriers_do_not_free_the_unit():
+    read, op = "v_mov_b32_e32 v120, v15", "v_mfma_f32_32x32x2_f32"
+    assert found(matrix(op, 0, 15), "s_waitcnt lgkmcnt(0)", matrix(op, 32, 47), "s_nop 0", read) == [read]
+    assert found(matrix(op, 0, 15), "s_waitcnt lgkmcnt(0)", matrix(op, 32, 47), "s_nop 1", read) == []
+
+
+def test_a_taken_branch_is_one_state():
+    read = "v_mov_b32_e32 v120, v15"
+    for need, op in ((12, "v_mfma_f32_32x32x16_bf16"), (18, "v_mfma_f32_32x32x2_f32")):
+        for branch in ("s_branch .LBB0_2", "s_cbranch_scc1 .LBB0_2"):
+            lines = lambda n: (matrix(op, 0, 15), *["s_nop 0"] * n, branch, "s_nop 15", "s_nop 15", ".LBB0_2:", read)
+            assert found(*lines(need - 1)) == [] and found(*lines(need - 2)) == [read]
