@@ -98,7 +98,8 @@ def mfma_hazards(asm_text: str) -> list:
     as one each.  The hardware does not: a sum read that way was the one before.  Follows every path through
     every function with the distance of each register from the matrix instruction that wrote it.
     Returns a list of (function, line number, instruction)."""
-    # (state: register -> (states since its instruction, states needed); None -> the same of the matrix unit)
+    # (state: register -> (states since its instruction, states needed); None -> the same of the matrix unit.  Where paths meet, the
+    # register that lacks more states counts, and the unit that is free sooner.)
     functions, name, block = {}, None, None
     for ln, raw in enumerate(asm_text.splitlines(), 1):
         line = raw.split(";")[0].strip()
@@ -123,10 +124,17 @@ def mfma_hazards(asm_text: str) -> list:
             if entry[to] is None:
                 entry[to] = dict(state)
             else:
-                nearer = {r: v for r, v in state.items() if r not in entry[to] or v[1] - v[0] > entry[to][r][1] - entry[to][r][0]}
-                if not nearer:
+                nearer = {r: v for r, v in state.items()
+                          if r is not None and (r not in entry[to] or v[1] - v[0] > entry[to][r][1] - entry[to][r][0])}
+                lacks = lambda s: s[None][1] - s[None][0] if None in s else 0
+                sooner = lacks(state) < lacks(entry[to])
+                if not nearer and not sooner:
                     return
                 entry[to].update(nearer)
+                if sooner:
+                    entry[to].pop(None)
+                    if None in state:
+                        entry[to][None] = state[None]
             work.append(to)
 
         while work:

@@ -86,3 +86,17 @@ def test_a_taken_branch_is_one_state():
         for branch in ("s_branch .LBB0_2", "s_cbranch_scc1 .LBB0_2"):
             lines = lambda n: (matrix(op, 0, 15), *["s_nop 0"] * n, branch, "s_nop 15", "s_nop 15", ".LBB0_2:", read)
             assert found(*lines(need - 1)) == [] and found(*lines(need - 2)) == [read]
+
+
+@pytest.mark.parametrize("swap", [False, True])
+def test_where_paths_meet_the_unit_is_the_one_that_is_free_sooner(swap):
+    """On one path the first sum's instruction is four states ago, on the other another instruction has the unit for long: the matrix instruction
+    behind them waits for no one on the first path."""
+    read, short, long = "v_mov_b32_e32 v120, v3", matrix("v_mfma_f32_16x16x4_f32", 0, 3), matrix("v_mfma_f32_32x32x2_f32", 32, 47)
+    near = [short, "s_nop 2"]                          # and the branch: four states, four to go for the unit, six for the sum
+    busy = [short, "s_nop 15", long]
+    one, other = (busy, near) if swap else (near, busy)
+    join = [".LBB0_9:", matrix("v_mfma_f32_16x16x4_f32", 64, 67)]
+    paths = lambda n: ["s_cbranch_scc1 .LBB0_5", *one, "s_branch .LBB0_9", ".LBB0_5:", *other, "s_branch .LBB0_9", *join, *["s_nop 0"] * n, read]
+    assert found(*near, "s_nop 0", join[1], "s_nop 0", read) == [read]         # the first path alone: two states are missing
+    assert found(*paths(1)) == [read] and found(*paths(2)) == []
