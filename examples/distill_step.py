@@ -101,7 +101,8 @@ class Student:
         grad = {name: None if is_frozen[name] else g for name, g in self.grad.items()}
 
         def linear(names, X, dY):
-            """The layers' dW; the gradient of the input that they share."""
+            """The layers' dW; the gradient of the input that they share.  (One product for them all, tf_stage_backward_shared, in bf16 takes
+            only the sizes of the matrix-core kernel, and these tokens and widths may be any.)"""
             dX = [torch.empty_like(X) for _ in names]
             tf.tf_stage_backward(ctx, [self.shapes[i] for i in names], T, io, [w[i] for i in names], [X] * len(names), dY,
                                  [is_frozen[i] for i in names], dX, [self.grad[i] for i in names], tf.TF_F32)

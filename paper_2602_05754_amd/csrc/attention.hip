@@ -16,8 +16,11 @@
 //               dk^T = Q^T dS.  A block takes one or more query heads of a group; where they are not all, their sums
 //               are added by a kernel of their own, in order: no atomics, and the same call gives the same bits.
 //
-// P and dS are rounded to bf16 for the second products (bf16 inputs); sums, statistics and the factors
-// in between are 32-bit.
+// P and dS are rounded to bf16 for the second products (bf16 inputs), the type that the matrix cores take at sixteen times the rate of fp32;
+// sums, statistics and the factors in between are 32-bit.  The results' error, root mean square, is 1.25 to 1.42 times that of 32-bit products.
+// What the rounding takes away as a product of its own makes it 1.00, and costs 28 to 34 % of the time (forward, 4096 tokens, heads of 128 and 64:
+// 152 196, 90 121; backward, heads of 64: 281 373) and registers that dk and dv of heads of 128 do not have; the gradients of short sequences
+// have it (add_rest()).
 //
 // Stages are filled by direct loads, rows past a sequence's end by its last row again: their scores are masked.
 // A masked score is a select, but a zero weight times an infinite or NaN row is NaN: a block whose results are not

@@ -9,8 +9,10 @@
 // the rest is read twice.  Each thread takes the running maximum and sum of its pieces as they arrive, so that the exponentials of
 // the sum are done by the time the row is there, as those of the gradient are while it is written; what is to be done for
 // the K entries is done while the row is on its way.  The K entries of p are put in by writing those elements again, behind a barrier.
-// us and logical GB/s (copies run at 5000), bf16, K = 32: 4096 rows of 65536 205, 5230 (two blocks to a compute unit); 2048 of 131072 239,
-// 4490 (one: a row fills the registers, and nothing is read while it is written); 2048 of 160000 291, 4500.
+// us and logical GB/s (copies run at 5000), bf16, K = 32: 4096 rows of 65536 207, 5180 (two blocks to a compute unit); 2048 of 131072 236,
+// 4540 (one: a row fills the registers, and nothing is read while it is written); 2048 of 160000 289, 4530.  The loss alone: 92, 129 (4160: one
+// block to a unit, as with the gradient).  fp32, 2048 rows of 32000: 106, alone 46.  Each entry is compared with all of its row, for words
+// that are named twice: 2048 rows of 32000 with K = 32, 256 and 1024 take 62, 93 and 580.
 // Exponentials are of (z - maximum) / tau, the difference first: z / tau of a word masked with the type's lowest value
 // need not be finite, and where q is large the difference is exact.  The loss adds up tau log p and tau log q for the same reason: log q of such
 // a word is not finite at a temperature below 1, tau^2 log q is.

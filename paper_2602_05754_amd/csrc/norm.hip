@@ -12,9 +12,9 @@
 // group of rows, a lane keeps the sums of its columns, and the blocks' partial sums are added by a second
 // kernel in the order of the blocks, so that the same call gives the same bits.
 //
-// us and GB/s of what has to move (copies run at 5000), forward | backward with the sums: bf16, 4096 columns, 4096 rows 13.7, 4910 |
-// 26, 3880 (of which the sums 4), 8192 rows 23.2, 5780 | 46.9, 4290; fp32, 2048 columns, 16384 rows 52.7, 5090 | 81.7, 4930.
-// Rows of an odd number of bf16 start at odd addresses, where a wide load takes longer: 2731 columns, 8192 rows 25.2, 3560 | 68.8, 1950.
+// us and GB/s of what has to move (copies run at 5000), forward | backward with the sums: bf16, 4096 columns, 4096 rows 13.5, 4970 |
+// 25.6, 3930 (of which the sums 4), 8192 rows 26.6, 5050 | 43.7, 4600; fp32, 2048 columns, 16384 rows 51.5, 5210 | 79.3, 5080.
+// Rows of an odd number of bf16 start at odd addresses, where a wide load takes longer: 2731 columns, 8192 rows 25.4, 3530 | 66.2, 2030.
 #include "row_device.h"
 
 #include <algorithm>

@@ -114,6 +114,8 @@ enum { kAttentionByRule = 0, kAttentionWide = 1, kAttentionNarrow = 2 };
 //   bf16, heads of 128   2 x 128,  64  7.6 6.9 | 30 24    1 x 512, 128  14.4 14.3 | 51 49    1 x 1000, 256  24 34 | 76 98    3 x 334, 288  14 27 | 54 66
 //   fp32, heads of 64    1 x 512, 128  43 26 | 169 81    1 x 1000, 256  78 73 | 318 225    3 x 334, 288  36 44 | 138 122    1 x 2048, 512  200 248 | 727 784
 // Of sequences up to 64 tokens there is nothing to share out in a forward pass (bf16, heads of 64 and 128, 64 tokens: 4.6 4.7, 5.4 6.1).
+// The blocks of all sequences are counted, and 256 is where equal ones part on the whole, not everywhere (fp32 backward, 3 x 334).  Nor does it
+// see uneven ones: of 934, 54 and 13 tokens (320 blocks, bf16, heads of 64) the kernels of 128 rows take 18.2 | 55.8, those of 32 16.2 | 47.6.
 bool attention_narrow(const tf_ctx* ctx, Dtype dtype, int d, bool backward, int32_t n_seqs, const int64_t* starts, int64_t heads) {
     if (!attention_has_wide(d, dtype)) return true;
     if (ctx->attention_route != kAttentionByRule) return ctx->attention_route == kAttentionNarrow;
