@@ -194,13 +194,25 @@ def check_generated_code(assembled: list) -> None:
 
 
 def build(verbose: bool = False) -> str:
+    """Compiles the library; what fails a check does not take its place."""
+    unchecked = LIB + ".unchecked"
+    try:
+        _build(unchecked, verbose)
+        os.replace(unchecked, LIB)
+    finally:
+        if os.path.exists(unchecked):
+            os.remove(unchecked)
+    return LIB
+
+
+def _build(library: str, verbose: bool) -> None:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     extra = os.environ.get("TF_BUILD_FLAGS", "").split()      # developer experiments
     with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(8) as pool:
         outputs = [os.path.join(objects, s + ".o") for s in SOURCES]
         compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
         cmds = [[hipcc] + compile_flags + extra + ["-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, outputs)]
-        link = [hipcc] + [f for f in HIPCC_FLAGS if not f.startswith("-R")] + extra + outputs + ["-o", LIB]
+        link = [hipcc] + [f for f in HIPCC_FLAGS if not f.startswith("-R")] + extra + outputs + ["-o", library]
         if verbose:
             print("\n".join(" ".join(c) for c in cmds + [link]), flush=True)
         run = lambda c: subprocess.run(c, capture_output=True, text=True)
@@ -232,7 +244,6 @@ def build(verbose: bool = False) -> str:
         if m and int(m.group(1)) != 0:
             raise RuntimeError(f"kernel {name} uses {m.group(1)} bytes/lane of scratch memory")
     check_generated_code(assembled)
-    return LIB
 
 
 if __name__ == "__main__":

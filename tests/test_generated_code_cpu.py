@@ -100,3 +100,38 @@ def test_where_paths_meet_the_unit_is_the_one_that_is_free_sooner(swap):
     paths = lambda n: ["s_cbranch_scc1 .LBB0_5", *one, "s_branch .LBB0_9", ".LBB0_5:", *other, "s_branch .LBB0_9", *join, *["s_nop 0"] * n, read]
     assert found(*near, "s_nop 0", join[1], "s_nop 0", read) == [read]         # the first path alone: two states are missing
     assert found(*paths(1)) == [read] and found(*paths(2)) == []
+
+
+FAKE_HIPCC = """#!/bin/sh
+out=
+while [ $# -gt 0 ]; do
+  if [ "$1" = -o ]; then out=$2; shift; fi
+  shift
+done
+if [ "$out" = - ]; then cat "$FAKE_ASSEMBLY"; exit 0; fi
+echo new > "$out"
+echo "a.hip:1:1: remark: Function Name: kernel_a [-Rpass-analysis=kernel-resource-usage]" >&2
+echo "a.hip:1:1: remark:     ScratchSize [bytes/lane]: $FAKE_SCRATCH [-Rpass-analysis=kernel-resource-usage]" >&2
+exit $FAKE_STATUS
+"""
+
+
+@pytest.mark.parametrize("scratch,lines,status,error", [("0", [MFMA, WAIT, READ], "0", None), ("8", [], "0", "scratch memory"), ("0", [MFMA, READ], "0", "too early"),
+                                                        ("0", [], "1", "hipcc failed")])
+def test_a_library_that_fails_a_check_takes_no_place(tmp_path, monkeypatch, scratch, lines, status, error):
+    from paper_2602_05754_amd import build
+    compiler, assembly, lib = tmp_path / "hipcc", tmp_path / "a.s", tmp_path / "libtf.so"
+    compiler.write_text(FAKE_HIPCC)
+    compiler.chmod(0o755)
+    assembly.write_text("kernel_a:\n" + "\n".join(lines) + "\ns_endpgm\n")
+    lib.write_text("old\n")
+    for name, value in (("HIPCC", str(compiler)), ("FAKE_ASSEMBLY", str(assembly)), ("FAKE_SCRATCH", scratch), ("FAKE_STATUS", status)):
+        monkeypatch.setenv(name, value)
+    monkeypatch.setattr(build, "LIB", str(lib))
+    if error is None:
+        assert build.build() == str(lib) and lib.read_text() == "new\n"
+    else:
+        with pytest.raises(RuntimeError, match=error):
+            build.build()
+        assert lib.read_text() == "old\n"
+    assert sorted(p.name for p in tmp_path.iterdir()) == ["a.s", "hipcc", "libtf.so"]
