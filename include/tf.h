@@ -572,7 +572,8 @@ double tf_actual_freeze_ratio(double r, int64_t t, int64_t T_m, int64_t T_f);
  * Scores, P and the sums are 32-bit; with TF_BF16, P and dS are rounded to bf16 as operands of the second
  * products, as o, dq, dk and dv are once at the end.  (In the gradients of sequences of up to 32 tokens, whatever they are
  * packed with, P and dS have 16 bits there: beside o's, only the result's own rounding is left.)  An infinite or NaN key, value, query or gradient
- * reaches the results that the formulas let it reach and no others.
+ * reaches the results that the formulas let it reach and no others.  A key with a score of -infinity has no weight; a query
+ * with no other has lse = -infinity, and its o is NaN.
  */
 int tf_attention_forward(tf_ctx* ctx, void* hip_stream, int32_t n_seqs, const int64_t* seq_starts, int64_t T,
                          int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, tf_dtype io_dtype,

@@ -25,7 +25,7 @@ def attention_forward(starts, q, k, v, scale):
                 s = scale * (k[a:i + 1, h // group] @ q[i, h])
                 m = s.max()
                 e = np.exp(s - m)
-                lse[i, h] = m + np.log(e.sum())
+                lse[i, h] = m + np.log(e.sum()) if m > -np.inf else m      # (nothing but -infinity: no result)
                 o[i, h] = (e / e.sum()) @ v[a:i + 1, h // group]
     return o, lse
 

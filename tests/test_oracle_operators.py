@@ -90,3 +90,17 @@ def test_distill_of_one_label_is_cross_entropy_and_of_itself_is_zero():
     assert np.allclose(loss, [lse[0] - z[0, 2], lse[1] - z[1, 0], lse[2] - z[2, 4]])
     loss, dz = op.distill_loss(z, np.tile(np.arange(5), (3, 1)), z + 3, None, 2.0, 1.0)   # teacher = student: no divergence
     assert np.allclose(loss, 0) and np.allclose(dz, 0)
+
+
+def test_attention_where_all_scores_are_minus_infinity():
+    """The first key is infinite, against all queries: the first query has nothing else, the others leave it out."""
+    rs = np.random.default_rng(3)
+    q, k, v = (rs.standard_normal((4, 1, 3)) for _ in range(3))
+    q[..., 1] = -1 - np.abs(q[..., 1])
+    k[0, 0, 1] = np.inf
+    with np.errstate(invalid="ignore"):
+        o, lse = op.attention_forward([0, 4], q, k, v, 0.5)
+    assert lse[0, 0] == -np.inf and np.isnan(o[0]).all()
+    for i in range(1, 4):
+        s = 0.5 * k[1:i + 1, 0] @ q[i, 0]
+        assert np.allclose(lse[i, 0], np.log(np.exp(s).sum())) and np.allclose(o[i, 0], np.exp(s) @ v[1:i + 1, 0] / np.exp(s).sum())
